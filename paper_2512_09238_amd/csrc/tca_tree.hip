@@ -72,7 +72,14 @@ struct TreeShape {
   SmallDiv by_region_groups, by_kv_groups, by_ring_units, by_GS, by_G;
 };
 
-// Partials of a sequence, D + 2 floats each: region unit by region unit its n GS queries, then for each KV head the units of its ring (the
+// A partial of T results: its reference (fp32 rows: a double, see tree_partial_f32_kernel), its sum and D columns.
+template <typename T> struct TreePartial {
+  using ref_t = std::conditional_t<sizeof(T) == 4, double, float>;
+  static constexpr int kSum = sizeof(ref_t) / 4, kColumns = 2 * kSum;      // where they lie, in floats
+};
+template <typename T, int D> constexpr int tree_partial_floats() { return D + TreePartial<T>::kColumns; }
+
+// Partials of a sequence: region unit by region unit its n GS queries, then for each KV head the units of its ring (the
 // last one with the nodes' own rows), n G queries each.  A query's number inside a unit: node * heads + head.
 __host__ __device__ __forceinline__ int64_t partials_of(const TreeShape& t) {
   return (int64_t)t.n * ((int64_t)t.GS * t.region_units + (int64_t)t.Hq * t.ring_units);
@@ -782,7 +789,8 @@ __device__ __forceinline__ float tree_exp2(double d) {
 }
 
 // The same for fp32 rows, which come from memory to the operands: a wave has tiles of 16 keys and the workgroup 16 queries.  Logits
-// (in units of ln 2) fp64 from v_mfma_f64_16x16x4, references whole numbers (exact in fp32, and through the merges); the
+// (in units of ln 2) fp64 from v_mfma_f64_16x16x4; references whole numbers, fp64 too, from the first tile to the last merge (the fp32
+// number next to a logit of 2^31 may be 128 away from it, and the weights with it infinite or nothing); the
 // product with V on v_mfma_f32_16x16x4, of tiles at the edges key by key on the vector ALU (a masked key's V row may be
 // anything).  lane = (kb = lane / 16, c = lane % 16): scores of the keys kb + 4 r against query c; of O^T the elements (D / 16) (4 kb + r) + s.
 // grid (units of all sequences, of 16 queries each); block 256
@@ -792,15 +800,17 @@ __global__ __launch_bounds__(kTreeThreads) void tree_partial_f32_kernel(
     const float* __restrict__ k_new, const float* __restrict__ v_new, float* __restrict__ part, TreeTables tt) {
   typedef double f64x4_t __attribute__((ext_vector_type(4)));
   constexpr int TK = 16, SB = D / 16;
+  constexpr int PF = tree_partial_floats<float, D>(), kSum = TreePartial<float>::kSum, kColumns = TreePartial<float>::kColumns;
   __shared__ float acc_s[kTreeWaves][16][D];
-  __shared__ float ms[kTreeWaves][16], ls[kTreeWaves][16];
+  __shared__ double ms[kTreeWaves][16];
+  __shared__ float ls[kTreeWaves][16];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), s = blockIdx.y;
   const int kb = lane >> 4, cq = lane & 15, n = th.n, w = th.w, Hkv = th.Hkv;
   const TreeUnit u = tree_unit(th, tt.unit0, s, blockIdx.x);
   const int64_t T = c.length[s];
   const TreeNode node = tree_node(lane < n ? parent[(size_t)s * n + lane] : -2);
   const int n_q = n * u.heads, q0 = u.group * 16;
-  float* const out = part + (u.first + q0) * (D + 2);
+  float* const out = part + (u.first + q0) * PF;
   const int x = min(q0 + cq, n_q - 1), i = u.ring ? th.by_G(x) : th.by_GS(x);
   const int exists = __shfl((int)node.there, i, kWave);                // (by all lanes)
   const bool there = q0 + cq < n_q && exists != 0;
@@ -832,7 +842,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_partial_f32_kernel(
   }
   n_rows = __builtin_amdgcn_readfirstlane(n_rows);
   if (n_rows <= 0 && node_rows == 0) {
-    if (tid < min(n_q - q0, 16)) { out[(size_t)tid * (D + 2)] = -INFINITY; out[(size_t)tid * (D + 2) + 1] = 0.f; }
+    if (tid < min(n_q - q0, 16)) { *reinterpret_cast<double*>(out + (size_t)tid * PF) = -INFINITY; out[(size_t)tid * PF + kSum] = 0.f; }
     return;
   }
   auto distance = [&](int r) { const int y = r - hidden; return y < 0 ? y + w : y >= w ? y - w : y; };
@@ -844,7 +854,8 @@ __global__ __launch_bounds__(kTreeThreads) void tree_partial_f32_kernel(
 #pragma unroll
     for (int e = 0; e < 4; ++e) qd[4 * t + e] = (double)v[e];
   }
-  float m = -INFINITY, l = 0.f;
+  double m = -INFINITY;
+  float l = 0.f;
   f32x4_t o[SB];
 #pragma unroll
   for (int s = 0; s < SB; ++s) o[s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -885,10 +896,10 @@ __global__ __launch_bounds__(kTreeThreads) void tree_partial_f32_kernel(
     }
     mx = fmax(mx, __shfl_xor(mx, 16, kWave));
     mx = fmax(mx, __shfl_xor(mx, 32, kWave));
-    const float m_new = fmaxf(m, ceilf((float)mx));
-    const float corr = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;
+    const double m_new = fmax(m, ceil(mx));
+    const float corr = m_new > m ? __builtin_amdgcn_exp2f((float)(m - m_new)) : 1.f;
     m = m_new;
-    const double ref = m == -INFINITY ? 0.0 : (double)m;
+    const double ref = m == -INFINITY ? 0.0 : m;
     float p[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[r] = see[r] && xs[r] != -INFINITY ? tree_exp2(xs[r] - ref) : 0.f;
@@ -939,19 +950,20 @@ __global__ __launch_bounds__(kTreeThreads) void tree_partial_f32_kernel(
   for (int y = tid; y < 16 * D; y += kTreeThreads) {
     const int qi = y / D, d = y % D;
     if (q0 + qi >= n_q) continue;
-    float M = -INFINITY;
+    double M = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < kTreeWaves; ++k) M = fmaxf(M, ms[k][qi]);
+    for (int k = 0; k < kTreeWaves; ++k) M = fmax(M, ms[k][qi]);
     double L = 0, a = 0;                         // (in fp32 the four parts' sums would add their roundings)
 #pragma unroll
     for (int k = 0; k < kTreeWaves; ++k)
       if (ls[k][qi] != 0.f) {
-        const float wgt = __builtin_amdgcn_exp2f(ms[k][qi] - M);
+        const float wgt = __builtin_amdgcn_exp2f((float)(ms[k][qi] - M));
         L += (double)ls[k][qi] * wgt;
         a += (double)acc_s[k][qi][d] * wgt;
       }
-    out[(size_t)qi * (D + 2) + 2 + d] = (float)a;
-    if (d == 0) { out[(size_t)qi * (D + 2)] = M; out[(size_t)qi * (D + 2) + 1] = (float)L; }
+    float* const row = out + (size_t)qi * PF;
+    row[kColumns + d] = (float)a;
+    if (d == 0) { *reinterpret_cast<double*>(row) = M; row[kSum] = (float)L; }
   }
 }
 
@@ -961,34 +973,35 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void tree_merge_kernel(const int32_t* __restrict__ parent, const float* __restrict__ part, T* __restrict__ O,
                                                          TreeShape th, SmallDiv by_Hq, TreeTables tt) {
   using sum_t = std::conditional_t<sizeof(T) == 4, double, float>;         // (as in the merge of a decode step)
-  constexpr int C = D / 64;
+  using ref_t = typename TreePartial<T>::ref_t;
+  constexpr int C = D / 64, PF = tree_partial_floats<T, D>(), kColumns = TreePartial<T>::kColumns;
   const int lane = threadIdx.x & 63, s = blockIdx.y, n = th.n;
   const int x = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (x >= n * th.Hq) return;
   const int up = lane < n ? parent[(size_t)s * n + lane] : -2;
   const int i = by_Hq(x), h = x - i * th.Hq, hs = th.by_GS(h), kvh = th.by_G(h);
   const int first = tt.unit0[hs], ns = tt.unit0[hs + 1] - first, n_slots = ns + th.ring_units;
-  const float* const seq = part + (size_t)s * partials_of(th) * (D + 2);
-  const float* const p_region = seq + ((size_t)first * n * th.GS + (size_t)i * th.GS + (h - hs * th.GS)) * (D + 2);
-  const float* const p_kv = seq + ((size_t)n * th.GS * th.region_units + (size_t)kvh * th.ring_units * n * th.G + (size_t)i * th.G + (h - kvh * th.G)) * (D + 2);
-  const size_t step_region = (size_t)n * th.GS * (D + 2), step_kv = (size_t)n * th.G * (D + 2);
+  const float* const seq = part + (size_t)s * partials_of(th) * PF;
+  const float* const p_region = seq + ((size_t)first * n * th.GS + (size_t)i * th.GS + (h - hs * th.GS)) * PF;
+  const float* const p_kv = seq + ((size_t)n * th.GS * th.region_units + (size_t)kvh * th.ring_units * n * th.G + (size_t)i * th.G + (h - kvh * th.G)) * PF;
+  const size_t step_region = (size_t)n * th.GS * PF, step_kv = (size_t)n * th.G * PF;
   auto partial_at = [&](int k) { return k < ns ? p_region + k * step_region : p_kv + (size_t)(k - ns) * step_kv; };
   T* const row = O + (((size_t)s * n + i) * th.Hq + h) * D + lane * C;
-  float M = -INFINITY;
+  ref_t M = -INFINITY;
   sum_t L = 0, a[C];
 #pragma unroll
   for (int e = 0; e < C; ++e) a[e] = 0;
   for (int k0 = 0; k0 < n_slots; k0 += 64) {
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (k0 + lane < n_slots) ml = *reinterpret_cast<const float2*>(partial_at(k0 + lane));
+    struct __attribute__((aligned(8))) { ref_t m; float l; } ml = {-INFINITY, 0.f};
+    if (k0 + lane < n_slots) ml = *reinterpret_cast<const decltype(ml)*>(partial_at(k0 + lane));
     if (k0 == 0 && !__shfl((int)tree_node(up).there, i, kWave)) return;           // (while they are on their way)
-    float top = ml.y != 0.f ? ml.x : -INFINITY;                         // (a NaN sum is no empty partial)
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
-    const float m_new = fmaxf(M, top);
-    const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - m_new);
-    const float wgt = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - m_new) : 0.f;
-    const bool some = ml.y != 0.f;
-    L = L * corr + group_sum(some ? (sum_t)ml.y * wgt : (sum_t)0, kWave);
+    const bool some = ml.l != 0.f;                                      // (a NaN sum is no empty partial)
+    ref_t top = some ? ml.m : -INFINITY;
+    for (int o = 32; o > 0; o >>= 1) top = fmax(top, __shfl_xor(top, o, kWave));
+    const ref_t m_new = fmax(M, top);
+    const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((float)(M - m_new));
+    const float wgt = some ? __builtin_amdgcn_exp2f((float)(ml.m - m_new)) : 0.f;
+    L = L * corr + group_sum(some ? (sum_t)ml.l * wgt : (sum_t)0, kWave);
 #pragma unroll
     for (int e = 0; e < C; ++e) a[e] *= corr;
     M = m_new;
@@ -1005,7 +1018,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const int32_t* __restri
           const int k = __builtin_ctzll(left);
           left &= left - 1;
           wk[y] = __shfl(wgt, k, kWave);
-          const float* const src = partial_at(k0 + k) + 2 + lane * C;
+          const float* const src = partial_at(k0 + k) + kColumns + lane * C;
           if constexpr (C == 2) { const float2 z = *reinterpret_cast<const float2*>(src); v[y][0] = z.x; v[y][1] = z.y; }
           else v[y][0] = *src;
         }
@@ -1055,7 +1068,10 @@ static int64_t set_tree_chunk(TreeShape& th, TreeTables& tt, const tca_params* p
   return run * th.region_groups + (int64_t)th.Hkv * th.ring_units * th.kv_groups;
 }
 
-static size_t tree_bytes(const tca_params* prm, int64_t partials) { return align_up((size_t)partials * (prm->head_dim + 2) * sizeof(float), 256); }
+static size_t tree_bytes(const tca_params* prm, int64_t partials) {
+  const int head = prm->dtype == TCA_F32 ? TreePartial<float>::kColumns : TreePartial<bf16_t>::kColumns;
+  return align_up((size_t)partials * (prm->head_dim + head) * sizeof(float), 256);
+}
 
 // The chunk length of a step, as far as its partials have room: the shortest with which all units run at a time, two on a CU, or if none
 // does the shortest that comes to kTreeUnits, or the full one.  A unit's start and end take about 8 us, as long as 160 rows of its share of
