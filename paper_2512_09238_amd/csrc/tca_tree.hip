@@ -31,6 +31,8 @@
 // inside the window iff that distance is over e.  Nodes: the path's bits.  Only tiles at these edges evaluate a mask.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 #include "tca_tree.h"
@@ -430,7 +432,8 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
   for (int sl = 0; sl < DS; ++sl) vfa[sl] = tree_v_off<D>(vr, 4 * sl + 2 * (cc >> 4) + ((cc >> 1) & 1)) + (cc & 1) * 8;
 
   f32x16_t o[DS];
-  float m = -INFINITY, l = 0.f;                  // m: in base-2 units
+  float m = -INFINITY, l = 0.f;                  // m: as the scores are (FP8: in base-2 units; bf16: before the factor sl2e)
+  const float unit = kFp8 ? 1.f : sl2e;
 #pragma unroll
   for (int sl = 0; sl < DS; ++sl)
 #pragma unroll
@@ -475,9 +478,9 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
 #pragma unroll
     for (int r = 1; r < 4 * SUB; ++r) m4[0] = fmaxf(m4[0], m4[r]);
     const float mx = half_max(m4[0]);
-    const float m_new = fmaxf(m, kFp8 ? mx : mx * sl2e);
+    const float m_new = fmaxf(m, mx);
     if (__any(m_new > m)) {
-      const float alpha = m_new > m ? __builtin_amdgcn_exp2f(m - m_new) : 1.f;          // 0 while m = -inf
+      const float alpha = m_new > m ? __builtin_amdgcn_exp2f((m - m_new) * unit) : 1.f;          // 0 while m = -inf
       l *= alpha;
 #pragma unroll
       for (int sl = 0; sl < DS; ++sl)
@@ -485,7 +488,20 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
         for (int r = 0; r < 16; ++r) o[sl][r] *= alpha;
       m = m_new;
     }
-    const float ref = m_new == -INFINITY ? 0.f : m_new;                // (keys of -inf only: no weight)
+    const float top = m_new == -INFINITY ? 0.f : m_new;                // (keys of -inf only: no weight)
+    // bf16: a weight is exp2(fma(score, sl2e, -ref)), one instruction less than from the difference to the maximum.  ref is rounded, which
+    // is up to 2^-15 of a unit for references up to 2^10; those beyond take the difference (from 2^31 on a weight came out infinite,
+    // or none was left).
+    float ref = top * unit;
+    if constexpr (!kFp8) {
+      if (__any(fabsf(ref) > 0x1p10f)) {
+#pragma unroll
+        for (int sub = 0; sub < SUB; ++sub)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sv[sub][r] -= top;
+        ref = 0.f;
+      }
+    }
     // The largest term of a query is 1 up to the rounding of its logit; the sum takes the fp32 terms, the product the terms rounded
     // to bf16, which is where the outputs' error of half a step of bf16 per term comes from.
     bf16x8_t pf[SUB][2];
@@ -724,7 +740,7 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
   f32x4_t* const po = reinterpret_cast<f32x4_t*>(lds);
   const float lt = half_sum(l);
   __syncthreads();
-  if (hh == 0) { ms[wv * 32 + cc] = m; ls[wv * 32 + cc] = lt; }
+  if (hh == 0) { ms[wv * 32 + cc] = m * unit; ls[wv * 32 + cc] = lt; }
 #pragma unroll
   for (int sl = 0; sl < DS; ++sl)
 #pragma unroll
@@ -1153,7 +1169,7 @@ extern "C" int tca_decode_tree(const tca_params* prm, const tca_cache* cache, co
                            (const int32_t*)cache->idx, (const KV*)cache->Kg, (const KV*)cache->Vg, (const int32_t*)cache->n_rows,
                            (const KV*)cache->ringK, (const KV*)cache->ringV, (const int64_t*)cache->length, (const float*)cache->Kg_scale,
                            (const float*)cache->Vg_scale, (const float*)cache->ringK_scale, (const float*)cache->ringV_scale, cache->cap_rows,
-                           (float)sl2e, th.n, th.Hq, th.Hkv, th.G, th.GS, th.w, th.chunk, th.ring_units, th.region_units, th.region_groups,
+                           std::max((float)sl2e, FLT_MIN), th.n, th.Hq, th.Hkv, th.G, th.GS, th.w, th.chunk, th.ring_units, th.region_units, th.region_groups,
                            th.kv_groups, th.by_region_groups, th.by_kv_groups, th.by_ring_units, th.by_GS, th.by_G, tt);
       };
       switch (groups_of(prm, n * th.GS) * 8 + groups_of(prm, n * th.G)) {

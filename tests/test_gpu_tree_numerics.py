@@ -73,7 +73,8 @@ def ties_far_above(tb, bufs, case, lengths, n, size, seed):
 
 # size times sqrt(d) log2 e in the middle: 2^24.5 .. 2^38, where neighbours in fp32 are 2 to 16384 apart, and a size of no trouble
 @pytest.mark.parametrize("size", [1.0, 2.0 ** 21, 2.0 ** 27, 2.0 ** 29, 2.0 ** 31, 2.0 ** 34])
-@pytest.mark.parametrize("rows,d,share", [("f32", 128, False), ("f32", 64, True)])
+@pytest.mark.parametrize("rows,d,share", [("f32", 128, False), ("f32", 64, True), ("bf16", 128, False), ("bf16", 64, True), ("fp8", 128, True),
+                                          ("fp8", 64, False)])
 def test_logits_of_any_size(tb, bufs, rows, d, share, size):
     case = shape(8, 2, d, 16, 160, rows, share)
     prm, c, q, k, v, parent = ties_far_above(tb, bufs, case, (2600, 300, 31), 11, size, 700)
