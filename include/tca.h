@@ -364,7 +364,7 @@ int tca_decode_static(const tca_params* prm, const tca_cache* cache, const int64
  * max(0,P-w+1) .. T-1, to its ancestors and to itself: what a decode step of its path would attend
  * to.  Rows of O without a node are left as they are.  The cache is only read.  q, k_new, v_new and,
  * for both calls, the cache's row arrays (Kg, Vg, ringK, ringV) must be 16-byte aligned.  bf16:
- * products of bf16 numbers, softmax and sums fp32, the softmax weights rounded to bf16 for the product
+ * products of bf16 numbers, softmax and sums fp32, the softmax weights held to 2^-17 of themselves for the product
  * with V.  fp32: fp64 logits, fp32 exponentials and sums.  TCA_KV_FP8: the nodes' K and V rows are
  * read as the cache would give them back.  ws_bytes: tca_decode_tree_workspace_bytes(), max_head_rows
  * as for tca_decode; calls that overlap in time (streams, replays of two graphs) take a workspace each.

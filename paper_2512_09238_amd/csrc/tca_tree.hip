@@ -9,21 +9,22 @@
 //             Each wave keeps an online softmax of its own; they are merged into one (reference, sum, acc[D]) partial per query.
 //   merge   : a wave per node and query head merges the partials of its region and of its KV head's ring.
 //
-// Up to 64 queries a row the memory is the bound: a row of K and V (512 bytes at d = 128, bf16) takes 64 x 512 flops, an eighth of
+// Up to 64 queries a row the memory is the bound: a row of K and V (512 bytes at d = 128, bf16) takes 64 x 768 flops, a fifth of
 // what the matrix cores do in the time that its bytes take.  So the shape follows the loads: tiles are copied straight into LDS ahead
 // of their use, a wave with a tile of its own needs no barrier, and two workgroups a CU cover each other's start and end.  32 heads,
-// d = 128, budgets of 27 % on average, box to box: 64 nodes over 16 x 100000 tokens 0.92 to 1.00 ms, 4.9 to 5.3 TB/s; 8 over 16 x
-// 60000 5.6 TB/s; 32 over 8 x 30000 165 to 178 us, 4.3 to 4.6 TB/s (a tenth of it in the rings, whose rows meet 128 queries); 5 over
-// 1 x 2000 16 us, of which the two launches, each a chain of waits, are all.  (A first shape, a wave with up to 64 queries and masks in
-// every tile: 1730 us, 283 us, 21 us.)
+// d = 128, budgets of 27 % on average: 64 nodes over 16 x 100000 tokens 1.01 to 1.02 ms, 4.9 TB/s; 8 over 16 x
+// 60000 514 us, 5.8 TB/s; 32 over 8 x 30000 173 us, 4.4 TB/s (a tenth of it in the rings, whose rows meet 128 queries); 5 over
+// 1 x 2000 15 us, of which the two launches, each a chain of waits, are all.  (A first shape, a wave with up to 64 queries and masks in
+// every tile: 1730 us, 283 us and 21 us for the first, third and last.)
 // With 128 queries a row, on the FP8 cache (half the bytes), the products and weights are the bound: 16 nodes of 8 heads over 12 x
-// 60000 tokens 187 to 200 us, where their bytes take 85 and their products 65.  A round of 128 queries and 64 keys takes two
-// workgroups of a CU 5200 cycles: products 2048, passage through LDS 2600, vector instructions 3000, each of them under the others of the
-// other workgroup in part.  (The products under the next 16 keys' weights, written out and fenced: 1 %.)
+// 60000 tokens 222 to 235 us, where their bytes take 85 and their products 95.  A round of 128 queries and 64 keys takes two
+// workgroups of a CU 6200 cycles: products 3070, passage through LDS 2600, vector instructions 3600, each of them under the others of the
+// other workgroup in part.
 //
 // Products as in the prefill kernel (v_mfma_f32_32x32x16_bf16; lane = (hh = lane / 32, c = lane % 32)):
 //   S^T = K Q^T  : A = K rows (key = c, 8 consecutive d), B = Q (query = c, same 8 d), C[key = 8 (r/4) + 4 hh + r%4][query = c]
-//   O^T = V^T P^T: B = P^T from the C registers, A = V^T (d = c, the same 8 keys) by transposing LDS reads
+//   O^T = V^T P^T: B = P^T from the C registers, A = V^T (d = c, the same 8 keys) by transposing LDS reads; P^T as two bf16 numbers a
+//   weight, a product each
 // A lane holds 16 keys of one query: maximum and sum are in-register reductions and one exchange between the halves.
 //
 // Visibility.  Node of depth e sits at T + e.  Region: idx ascends, so a query sees a prefix; the prefix of depth 0 is counted
@@ -502,9 +503,11 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
         ref = 0.f;
       }
     }
-    // The largest term of a query is 1 up to the rounding of its logit; the sum takes the fp32 terms, the product the terms rounded
-    // to bf16, which is where the outputs' error of half a step of bf16 per term comes from.
-    bf16x8_t pf[SUB][2];
+    // The sum takes the fp32 terms; the product takes each as two bf16 numbers, its leading bits and what they leave, together off by
+    // 2^-17 of it at most, so that an element whose terms cancel is as exact as from a decode step's fp32 weights.  (Leading bits alone:
+    // up to 50 times that error.  us without / with the second product: 32 nodes over 8 x 30000 tokens 172 / 173, 64 over 16 x 100000
+    // 985 / 1006; where products bind, 16 of 64 heads over 12 x 60000, FP8 and a shared selection, 189 / 222, 48 over 8 x 50000 247 / 291.)
+    bf16x8_t pf[SUB][2], pl[SUB][2];
     float lt[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int sub = 0; sub < SUB; ++sub) {
@@ -519,7 +522,9 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
           lt[e] += p;
           float pv = p;
           if constexpr (kFp8) pv = kEdge && x == -INFINITY ? 0.f : p * vs[e];           // the V row's scale rides on the weight
-          pf[sub][r >> 3][r & 7] = (__bf16)pv;
+          const __bf16 hi = (__bf16)pv;
+          pf[sub][r >> 3][r & 7] = hi;
+          pl[sub][r >> 3][r & 7] = (__bf16)(pv - (float)hi);
         }
       }
     }
@@ -528,10 +533,18 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
 #pragma unroll
     for (int g = 0; g < 2 * SUB; ++g)
 #pragma unroll
-      for (int sl = 0; sl < DS; ++sl) {
-        const unsigned char* at = vb + vfa[sl] + g * (16 * D * 2);
-        const bf16x4_t lo = tree_read_transposed(at), hi = tree_read_transposed(at + 8 * D * 2);
-        o[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), pf[g >> 1][g & 1], o[sl], 0, 0, 0);
+      for (int s2 = 0; s2 < DS; s2 += 2) {             // (two slices: a product waits for the one before it on the same sums)
+        bf16x8_t vt[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const unsigned char* at = vb + vfa[s2 + y] + g * (16 * D * 2);
+          const bf16x4_t lo = tree_read_transposed(at), hi = tree_read_transposed(at + 8 * D * 2);
+          vt[y] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) o[s2 + y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[y], pl[g >> 1][g & 1], o[s2 + y], 0, 0, 0);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) o[s2 + y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[y], pf[g >> 1][g & 1], o[s2 + y], 0, 0, 0);
       }
   };
 
@@ -1093,10 +1106,13 @@ static size_t tree_bytes(const tca_params* prm, int64_t partials) {
 // does the shortest that comes to kTreeUnits, or the full one.  A unit's start and end take about 8 us, as long as 160 rows of its share of
 // the memory's rate, so that many short units lose; one round of long ones has no last round, and where there are several
 // the last one should be short.  us with at most 512 / 1024 / 2048 units (32 heads, 8 KV heads, d = 128, bf16): 1 x 30000 tokens
-// and 16 nodes 30 / 39 / 55, 2 x 100000 and 64 142 / 153 / 159, 4 x 30000 and 8 87 / 88 / 94; more than 512 in any case: 8 x 30000
-// and 32 - / 181 / 177, 16 x 8000 and 24 (FP8) - / 132 / 126.  Where a region's rows meet more than 64 queries units are bound by
+// and 16 nodes 29 / 37 / 53, 2 x 100000 and 64 141 / 152 / 155, 4 x 30000 and 8 82 / 84 / 89; more than 512 in any case: 8 x 30000
+// and 32 199 / 180 / 174, 16 x 8000 and 24 (FP8) 221 / 143 / 134.  Where a region's rows meet more than 64 queries units are bound by
 // their products, and those of one round do not end together as those that share the memory do: kTreeBusy in any case.  Shared selection,
-// 512 / 1024 / 2048: 4 x 20000 and 16 (64 heads, FP8) 64 / 56 / 73, 8 x 50000 and 48 204 / 183 / 201.
+// 512 / 1024 / 2048: 4 x 20000 and 16 (64 heads, FP8) 70 / 57 / 69, 8 x 50000 and 48 (FP8) 225 / 218 / 228, on bf16 rows 189 / 202 / 220.
+// fp32 rows take the same numbers, whose units of 16 queries are one on a CU at d = 128: 1 x 5000 and 8 54 / 61 / 60, 1 x 20000 and 24 123 / 139 / 160,
+// 16 x 20000 and 8 765 / 765 / 691; 512 are enough for 4 x 12000 and 20, 369 / 304 / 289, and for 8 x 8000 and 16, 438 / 353 / 326, which more
+// would suit.
 static int64_t choose_tree_chunk(TreeShape& th, TreeTables& tt, const tca_params* prm, int batch, int n, size_t ws_bytes) {
   const bool busy = groups_of(prm, n * sel_group(prm)) == 4;
   for (const int most : {busy ? kTreeBusy : kTreeSlots, busy ? kTreeBusy : kTreeUnits})

@@ -1,4 +1,5 @@
-"""Drafted trees: logits of any size."""
+"""Drafted trees where the other tests' tolerances say little: logits of any size, weights in as many bits as a decode step holds them
+in."""
 import numpy as np
 import pytest
 import torch
@@ -92,3 +93,73 @@ def test_logits_of_any_size(tb, bufs, rows, d, share, size):
     off = np.abs(O - want) / tol
     print("worst error over tolerance %.3f" % off.max(), flush=True)
     assert off.max() <= 1.0
+
+
+# ------------------------------------------------------------------------------------------------- bits of weights --
+def visible(case, c, q, k, v, parent):
+    """Per node and head: (sequence, node, head), the weights of the rows that it sees and these rows of V in float64, and how far fp32
+    logits may be off (a sum of d products: d 2^-24 of its terms' magnitudes; fp32 rows have fp64 logits)."""
+    B, n, Hq, d = q.shape
+    Hs, Hkv, w = c.n_rows.shape[1], case["hkv"], case["w"]
+    qf, kf, vf, par = q.double().cpu().numpy(), R.stored(case, k), R.stored(case, v), parent.cpu().numpy()
+    for s in range(B):
+        T, idx = int(c.length[s]), c.idx[s].cpu().numpy()
+        Kg, Vg, rK, rV = (R.read_back(c, x, s) for x in ("Kg", "Vg", "ringK", "ringV"))
+        for i in range(n):
+            line = R.line_to(par[s], i)
+            P = T + len(line) - 1
+            old = np.arange(max(0, P - w + 1), T) % w
+            for h in range(Hq):
+                hs, kv = h // (Hq // Hs), h // (Hq // Hkv)
+                o = int(c.offs[hs])
+                at = o + np.nonzero(idx[o:o + int(c.n_rows[s, hs])] <= P - w)[0]
+                keys = np.concatenate([Kg[at], rK[kv, old], kf[s, line, kv]])
+                x = keys @ qf[s, i, h] / np.sqrt(d)
+                e = np.exp(x - x.max())
+                off = d * 2.0 ** -24 * (np.abs(keys) @ np.abs(qf[s, i, h])).max() / np.sqrt(d)
+                yield (s, i, h), e / e.sum(), np.concatenate([Vg[at], rV[kv, old], vf[s, line, kv]]), 0.0 if case["rows"] == "f32" else off
+
+
+def sharp(case, c, q, k, v, parent):
+    """(O, tolerance) in float64 where a weight is held in 16 bits or more (off by 2^-17 of itself): numerator and denominator twice the
+    logits' error, sums of N terms in fp32 and exponentials (8 times 2^-24), and the result's rounding."""
+    O, tol = np.empty(q.shape), np.empty(q.shape)
+    half = 2.0 ** -24 if case["rows"] == "f32" else 2.0 ** -8
+    for at, p, vals, off in visible(case, c, q, k, v, parent):
+        O[at] = p @ vals
+        tol[at] = half * np.abs(O[at]) + (2.0 ** -17 + 2 * off + 2 * (len(p) + 8) * 2.0 ** -24) * (p @ np.abs(vals))
+    return O, tol
+
+
+@pytest.mark.parametrize("rows,d,share,n", [("bf16", 128, False, 1), ("bf16", 64, True, 9), ("bf16", 64, False, 40), ("bf16", 128, True, 20),
+                                            ("bf16", 64, True, 64), ("fp8", 128, False, 1), ("fp8", 64, True, 9), ("fp8", 64, False, 40),
+                                            ("fp8", 128, True, 20), ("fp8", 64, True, 64), ("f32", 64, False, 9)])
+def test_weights_have_the_bits_of_a_decode_step(tb, bufs, rows, d, share, n):
+    """Elements that are near zero, where the terms cancel, show the weights' error bare of the result's rounding."""
+    case = shape(8, 2, d, 16, 160, rows, share)
+    prm, c = R.filled_cache(tb, bufs, case, (500, 170, 0), 721)
+    q, k, v, parent = R.draft(case, 3, n, 722, [forked(n)] * 3)
+    q = (q.float() / 3).to(q.dtype)
+    want, tol = sharp(case, c, q, k, v, parent)
+    O = attend(tb, bufs, prm, c, q, k, v, parent).double().cpu().numpy()
+    off = np.abs(O - want) / tol
+    print("worst error over tolerance %.3f" % off.max(), flush=True)
+    assert off.max() <= 1.0
+
+
+@pytest.mark.parametrize("rows,share", [("bf16", False), ("bf16", True), ("fp8", False), ("fp8", True), ("f32", False)])
+def test_a_tree_of_one_node_is_as_exact_as_a_decode_step(tb, bufs, rows, share):
+    case = shape(8, 2, 128, 16, 160, rows, share)
+    prm, c = R.filled_cache(tb, bufs, case, (900, 333), 731)
+    q, k, v, parent = R.draft(case, 2, 1, 732, [[-1]] * 2)
+    want, tol = sharp(case, c, q, k, v, parent)
+    O = attend(tb, bufs, prm, c, q, k, v, parent)
+    P = np.stack([tb.tca_config_from_budget(16, 1.0, 0.4)] * tb.tca_selection_heads(prm))
+    Od = torch.empty_like(q[:, 0])
+    tb.tca_decode(prm, c.view, c.offs, q[:, 0].contiguous(), k[:, 0].contiguous(), v[:, 0].contiguous(), P, Od,
+                  bufs.workspace(tb.tca_decode_workspace_bytes(prm, 2, c.max_head_rows)))
+    torch.cuda.synchronize()
+    for name, x in (("tree", O[:, 0]), ("decode", Od)):
+        off = np.abs(x.double().cpu().numpy() - want[:, 0]) / tol[:, 0]
+        print("%s: worst error over tolerance %.3f" % (name, off.max()), flush=True)
+        assert off.max() <= 1.0
