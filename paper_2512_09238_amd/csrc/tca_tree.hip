@@ -125,12 +125,12 @@ __device__ __forceinline__ void tree_copy16(__amdgpu_buffer_rsrc_t rsrc, int lan
 // references, sums, scales, flags.
 constexpr int kNW = 4;
 constexpr int tree_stages(int qg) { return qg == 1 ? 1 : 2; }
-template <typename KV, int D> constexpr int tree_tile_bytes(int qg) {
+template <int D> constexpr int tree_tile_bytes(int qg) {
   const int tiles = kNW / qg * tree_stages(qg) * 4 * tree_keys(qg) * D, results = kNW * 32 * D * 4;
   return tiles > results ? tiles : results;
 }
 template <typename KV, int D> constexpr int tree_lds_bytes(int qg) {
-  return tree_tile_bytes<KV, D>(qg) + kNW * 32 * 8 + (sizeof(KV) == 1 ? kNW / qg * 16 * tree_keys(qg) : 0) + kNW / qg * 16;
+  return tree_tile_bytes<D>(qg) + kNW * 32 * 8 + (sizeof(KV) == 1 ? kNW / qg * 16 * tree_keys(qg) : 0) + kNW / qg * 16;
 }
 
 // What a workgroup works on: blockIdx.x, the rings' units first.
@@ -248,7 +248,7 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
   const int hh = lane >> 5, cc = lane & 31;
   const int kg = wv / QG, qg = wv % QG;
   unsigned char* const mine = lds + kg * (STAGES * 2 * TB);
-  float* const extra = reinterpret_cast<float*>(lds + tree_tile_bytes<KV, D>(QG));
+  float* const extra = reinterpret_cast<float*>(lds + tree_tile_bytes<D>(QG));
   float* const ms = extra;                       // [NW][32]
   float* const ls = ms + NW * 32;
   float* const scales = ls + NW * 32;            // FP8: [KG][2 stages][K (times sl2e), V][TK]
@@ -611,25 +611,14 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
         copy_v(tile_of(i + 1), mine);
       }
     } else {
-      constexpr int kLoads = (STAGES - 2) * 2 * NL;                    // of later tiles, still on their way when a tile is worked on
-      static_assert(kLoads < 64, "six bits");
-      if (rounds > 0) {
-#pragma unroll
-        for (int i = 1; i < STAGES - 1; ++i) {
-          copy_k(tile_of(i), mine + i * (2 * TB));
-          copy_v(tile_of(i), mine + i * (2 * TB));
-        }
-      }
-      int st = 0;
+      static_assert(STAGES == 2, "the next tile into the other one");
 #pragma unroll 1
-      for (int i = 0; i < rounds; ++i) {
-        __builtin_amdgcn_s_waitcnt(0x0F70 | (kLoads & 15) | (kLoads >> 4 << 14));
+      for (int i = 0, st = 0; i < rounds; ++i, st ^= 1) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);
         sync();                                  // this tile has landed, and the one before has been worked on
-        const int ahead = st == 0 ? STAGES - 1 : st - 1;
-        copy_k(tile_of(i + STAGES - 1), mine + ahead * (2 * TB));
-        copy_v(tile_of(i + STAGES - 1), mine + ahead * (2 * TB));
+        copy_k(tile_of(i + 1), mine + (st ^ 1) * (2 * TB));
+        copy_v(tile_of(i + 1), mine + (st ^ 1) * (2 * TB));
         if (i * KG + kg < n_clear) work_tile(mine + st * (2 * TB), nullptr, std::false_type{}, all, nothing);
-        st = st + 1 == STAGES ? 0 : st + 1;
       }
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);          // nothing more is on its way into LDS
