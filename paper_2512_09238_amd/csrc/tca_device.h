@@ -303,4 +303,52 @@ struct GroupReduce {
 };
 
 
+// 2^d for a difference of logits: the whole part taken off in fp64, so that nothing is lost of the fraction.  (-inf and what
+// lies below 2^31 give zero, a NaN a NaN.)  Seven instructions where expf of the rounded difference takes fifteen.
+__device__ __forceinline__ float exp2_diff(double d) {
+  int n;
+  asm("v_cvt_i32_f64 %0, %1" : "=v"(n) : "v"(d));                    // (saturates)
+  return ldexpf(__builtin_amdgcn_exp2f((float)(d - (double)n)), n);
+}
+
+// Operands and results of the bf16 matrix instructions.
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
+typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
+
+// Max and sum over a value of a lane and of the one 32 lanes across, in both.
+__device__ __forceinline__ float half_max(float v) {
+  float a, b;
+  lane_pair<32>(v, a, b);
+  return fmaxf(a, b);
+}
+__device__ __forceinline__ float half_sum(float v) {
+  float a, b;
+  lane_pair<32>(v, a, b);
+  return a + b;
+}
+
+// bf16 tiles in LDS, a row of D elements per key.  XOR swizzle of a row's 16-byte chunks.  K (V^T likewise): the 32 lanes of a half read
+// one chunk column of 32 rows.  V: a half of a transposing read takes 64 bytes, four chunks, of rows 0 .. 3 or 4 .. 7, which fill the 64
+// banks once if the four chunks move together by the row (by two at a time, so that eight rows of 32 bytes fill them, every
+// read took twice as long: SQ_LDS_BANK_CONFLICT).
+template <int D> __device__ __forceinline__ int k_swz(int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); }
+template <int D> __device__ __forceinline__ int v_swz(int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
+// LDS byte offset of 16-byte chunk `ch` of K row r, of V row r
+template <int D> __device__ __forceinline__ int k_off(int r, int ch) { return r * (D * 2) + ((ch ^ k_swz<D>(r)) << 4); }
+template <int D> __device__ __forceinline__ int v_off(int r, int ch) { return r * (D * 2) + ((ch ^ v_swz<D>(r)) << 4); }
+
+// Four keys of this lane's column.  Without the __restrict__ the compiler takes the read for one that may meet the tile copies in
+// flight and waits for them first, in the middle of every step (prefill of 128K tokens: 7 % more cycles).  No such wait is needed: the
+// tile read has landed by a wait and a barrier before, and the copies in flight go to other places.
+__device__ __forceinline__ bf16x4_t read_transposed(const unsigned char* __restrict__ lds_src) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4_t*)lds_src);
+}
+
+// 16 bytes per lane, global -> LDS (lanes deposit at consecutive addresses from lds_dst on); lane_off: the
+// lane's byte offset into the buffer, tile_off: a scalar byte offset on top
+__device__ __forceinline__ void copy16_to_lds(__amdgpu_buffer_rsrc_t rsrc, int lane_off, int tile_off, unsigned char* lds_dst) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds_dst, 16, lane_off, tile_off, 0, 0);
+}
+
 }  // namespace tca

@@ -49,9 +49,6 @@
 #include "tca_prefill.h"
 
 namespace tca {
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
-typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kBN = 64;              // keys per tile
@@ -226,33 +223,8 @@ __host__ __device__ __forceinline__ int pair_up(int u, int n) {
   return (u & 32) ? b + len - 1 - (u - b) : u;
 }
 
-// Cross-half exchange: returns max over the two 32-lane halves, in every lane.
-__device__ __forceinline__ float half_max(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float half_sum(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// XOR swizzle of a row's 16-byte chunks.  K, V^T: the 32 lanes of a half read one chunk column of 32 rows.  V: a half of a
-// transposing read takes 64 bytes, four chunks, of rows 0 .. 3 or 4 .. 7, which fill the 64 banks once if the four chunks
-// move together by the row (by two at a time, so that eight rows of 32 bytes fill them, every read took twice as long:
-// SQ_LDS_BANK_CONFLICT).
-template <int D> __device__ __forceinline__ int k_swz(int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); }
-template <int D> __device__ __forceinline__ int v_swz(int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
-// LDS byte offset of 16-byte chunk `ch` of K row r, of V^T row dd
-template <int D> __device__ __forceinline__ int k_off(int r, int ch) { return r * (D * 2) + ((ch ^ k_swz<D>(r)) << 4); }
+// LDS byte offset of 16-byte chunk `ch` of V^T row dd (swizzled as K's)
 __device__ __forceinline__ int vt_off(int dd, int ch) { return dd * (kBN * 2) + ((ch ^ ((dd >> 1) & 7)) << 4); }
-
-// Four keys of this lane's column (see vfa).  Without the __restrict__ the compiler takes the read for one that may meet
-// the tile copies in flight and waits for them first, in the middle of every step (128K tokens: 7 % more cycles).  No such wait
-// is needed: the tile read has landed by the wait and the barrier of the step before, and the copies in flight go to
-// other places of the ring.
-__device__ __forceinline__ bf16x4_t read_transposed(const unsigned char* __restrict__ lds_src) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4_t*)lds_src);
-}
 
 // Tile copies go global -> LDS directly (buffer loads with the LDS modifier: no
 // staging registers, no ds_write).  Every lane of a wave-load deposits 16 bytes at
@@ -287,12 +259,6 @@ struct TileCopy {
     return (dd * kBN + (pch ^ ((dd >> 1) & 7)) * 8) * 2;
   }
 };
-
-__device__ __forceinline__ void copy16_to_lds(__amdgpu_buffer_rsrc_t rsrc, int lane_off, int tile_off,
-                                              unsigned char* lds_dst) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds_dst, 16, lane_off,
-                                           tile_off, 0, 0);
-}
 
 // Software pipeline over the tiles of a workgroup (tile t = 0 .. n_tiles-1: first the
 // n_gt tiles of the head's compacted region, then the dense tiles of the window).  A wave

@@ -32,14 +32,6 @@ namespace tca {
 
 constexpr int row_threads(int kg) { return kg == 8 ? 512 : 256; }
 
-// 2^d for a difference of logits: the whole part taken off in fp64, so that nothing is lost of the fraction.  (-inf and what
-// lies below 2^31 give zero, a NaN a NaN.)  Seven instructions where expf of the rounded difference takes fifteen.
-__device__ __forceinline__ float exp2_diff(double d) {
-  int n;
-  asm("v_cvt_i32_f64 %0, %1" : "=v"(n) : "v"(d));                    // (saturates)
-  return ldexpf(__builtin_amdgcn_exp2f((float)(d - (double)n)), n);
-}
-
 struct HeadOffs { int64_t offs[TCA_MAX_HEADS + 1]; };
 
 // grid (query tiles * Hq), longest query tiles first, heads inside; block 256, 512 with KG = 8

@@ -25,9 +25,6 @@
 
 namespace tca {
 
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
-typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
 
 constexpr int kPK = 64;                          // the hidden size must be a multiple of this
 
@@ -39,14 +36,6 @@ struct QkvOut {
   int64_t head_stride[3], token_stride[3];
   int first_head[4];                             // part p holds the heads [first_head[p], first_head[p+1])
 };
-
-// 16 bytes per lane, global -> LDS (lanes deposit at consecutive addresses from lds_dst on); lane_off: the
-// lane's byte offset into the buffer, tile_off: a scalar byte offset on top
-__device__ __forceinline__ void copy16_to_lds(__amdgpu_buffer_rsrc_t rsrc, int lane_off, int tile_off,
-                                              unsigned char* lds_dst) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds_dst, 16, lane_off,
-                                           tile_off, 0, 0);
-}
 
 __device__ __forceinline__ int part_of_head(const QkvOut& o, int hg) { return hg < o.first_head[1] ? 0 : hg < o.first_head[2] ? 1 : 2; }
 

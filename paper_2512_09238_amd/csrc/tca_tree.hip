@@ -40,9 +40,6 @@
 
 namespace tca {
 
-typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
-typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kTreeThreads = 256;
@@ -88,38 +85,8 @@ __host__ __device__ __forceinline__ int64_t partials_of(const TreeShape& t) {
   return (int64_t)t.n * ((int64_t)t.GS * t.region_units + (int64_t)t.Hq * t.ring_units);
 }
 
-__device__ __forceinline__ float half_max(float v) {
-  float a, b;
-  lane_pair<32>(v, a, b);
-  return fmaxf(a, b);
-}
-__device__ __forceinline__ float half_sum(float v) {
-  float a, b;
-  lane_pair<32>(v, a, b);
-  return a + b;
-}
-
-// LDS tiles: a row per key, its 16-byte chunks swizzled by the row as in the prefill kernel (K for 16-byte reads of one chunk
-// column of 32 rows, V for transposing reads of four chunks of four rows).
-template <int D> __device__ __forceinline__ int tree_k_off(int r, int ch) {
-  const int swz = D == 128 ? (r & 15) : ((r >> 1) & 7);
-  return r * (D * 2) + ((ch ^ swz) << 4);
-}
-template <int D> __device__ __forceinline__ int tree_v_off(int r, int ch) {
-  const int swz = D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2;
-  return r * (D * 2) + ((ch ^ swz) << 4);
-}
-// (restricted: without an alias scope the compiler takes the reads for ones that may meet the tile copies in flight, and waits for those
-// first; the copies go to other stages)
+// (restricted as in read_transposed)
 __device__ __forceinline__ bf16x8_t tree_read16(const unsigned char* __restrict__ lds_src) { return *reinterpret_cast<const bf16x8_t*>(lds_src); }
-__device__ __forceinline__ bf16x4_t tree_read_transposed(const unsigned char* __restrict__ lds_src) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4_t*)lds_src);
-}
-
-// 16 bytes a lane straight into LDS (the lanes' places there follow each other)
-__device__ __forceinline__ void tree_copy16(__amdgpu_buffer_rsrc_t rsrc, int lane_off, int tile_off, unsigned char* lds_dst) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds_dst, 16, lane_off, tile_off, 0, 0);
-}
 
 // Waves of a workgroup, and its LDS: the tiles of its groups of waves, in stages (in their place at the end the waves' results); then
 // references, sums, scales, flags.
@@ -302,16 +269,16 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
 #pragma unroll
   for (int j = 0; j < NL; ++j) {
     const int cid = (j * QG + qg) * 64 + lane, r = cid / CPR, ch = cid % CPR;
-    klo[j] = tree_k_off<D>(r, ch);
-    vlo[j] = tree_v_off<D>(r, ch);
+    klo[j] = k_off<D>(r, ch);
+    vlo[j] = v_off<D>(r, ch);
   }
   auto copy_k = [&](int t, unsigned char* dst) {
 #pragma unroll
-    for (int j = 0; j < NL; ++j) tree_copy16(krs, klo[j], t * TB, dst + (j * QG + qg) * 1024);
+    for (int j = 0; j < NL; ++j) copy16_to_lds(krs, klo[j], t * TB, dst + (j * QG + qg) * 1024);
   };
   auto copy_v = [&](int t, unsigned char* dst) {
 #pragma unroll
-    for (int j = 0; j < NL; ++j) tree_copy16(vrs, vlo[j], t * TB, dst + TB + (j * QG + qg) * 1024);
+    for (int j = 0; j < NL; ++j) copy16_to_lds(vrs, vlo[j], t * TB, dst + TB + (j * QG + qg) * 1024);
   };
   // FP8: as codes in registers, from there as bf16 numbers (which hold every code) into LDS
   auto bf16_of_codes = [](uint32_t lo, uint32_t hi) {
@@ -345,10 +312,10 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
     for (int j = 0; j < NC; ++j) {
       const int cid = place(j), r = cid / (D / 16), ch = 2 * (cid % (D / 16));
       if (NC * QG * 64 == TK * D / 16 || cid < TK * D / 16) {
-        *reinterpret_cast<raw16_t*>(dst + tree_k_off<D>(r, ch)) = bf16_of_codes(x.k[j].x, x.k[j].y);
-        *reinterpret_cast<raw16_t*>(dst + tree_k_off<D>(r, ch + 1)) = bf16_of_codes(x.k[j].z, x.k[j].w);
-        *reinterpret_cast<raw16_t*>(dst + TB + tree_v_off<D>(r, ch)) = bf16_of_codes(x.v[j].x, x.v[j].y);
-        *reinterpret_cast<raw16_t*>(dst + TB + tree_v_off<D>(r, ch + 1)) = bf16_of_codes(x.v[j].z, x.v[j].w);
+        *reinterpret_cast<raw16_t*>(dst + k_off<D>(r, ch)) = bf16_of_codes(x.k[j].x, x.k[j].y);
+        *reinterpret_cast<raw16_t*>(dst + k_off<D>(r, ch + 1)) = bf16_of_codes(x.k[j].z, x.k[j].w);
+        *reinterpret_cast<raw16_t*>(dst + TB + v_off<D>(r, ch)) = bf16_of_codes(x.v[j].x, x.v[j].y);
+        *reinterpret_cast<raw16_t*>(dst + TB + v_off<D>(r, ch + 1)) = bf16_of_codes(x.v[j].z, x.v[j].w);
       }
     }
     if constexpr (TK == 32) {
@@ -427,10 +394,10 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
   // per-lane LDS offsets of the fragments inside a tile
   int kfa[KK], vfa[DS];
 #pragma unroll
-  for (int kk = 0; kk < KK; ++kk) kfa[kk] = tree_k_off<D>(cc, 2 * kk + hh);
+  for (int kk = 0; kk < KK; ++kk) kfa[kk] = k_off<D>(cc, 2 * kk + hh);
   const int vr = 4 * hh + ((cc >> 2) & 3);       // what a lane addresses: 4 columns of a key; what it receives: a column of 4 keys
 #pragma unroll
-  for (int sl = 0; sl < DS; ++sl) vfa[sl] = tree_v_off<D>(vr, 4 * sl + 2 * (cc >> 4) + ((cc >> 1) & 1)) + (cc & 1) * 8;
+  for (int sl = 0; sl < DS; ++sl) vfa[sl] = v_off<D>(vr, 4 * sl + 2 * (cc >> 4) + ((cc >> 1) & 1)) + (cc & 1) * 8;
 
   f32x16_t o[DS];
   float m = -INFINITY, l = 0.f;                  // m: as the scores are (FP8: in base-2 units; bf16: before the factor sl2e)
@@ -538,7 +505,7 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const unsigned char* at = vb + vfa[s2 + y] + g * (16 * D * 2);
-          const bf16x4_t lo = tree_read_transposed(at), hi = tree_read_transposed(at + 8 * D * 2);
+          const bf16x4_t lo = read_transposed(at), hi = read_transposed(at + 8 * D * 2);
           vt[y] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         }
 #pragma unroll
@@ -696,8 +663,8 @@ __device__ __forceinline__ void tree_body(const TreeCache<KV>& c, const TreeShap
             vw[j][x] &= (lo ? 0xFFFF0000u : 0xFFFFFFFFu) & (hi ? 0x0000FFFFu : 0xFFFFFFFFu);
           }
           if (bad) atomicOr(&odd[(i & 1) * KG + kg], 1ull << r);
-          *reinterpret_cast<raw16_t*>(mine + tree_k_off<D>(r, ch)) = kr[j];
-          *reinterpret_cast<raw16_t*>(mine + TB + tree_v_off<D>(r, ch)) = vw[j];
+          *reinterpret_cast<raw16_t*>(mine + k_off<D>(r, ch)) = kr[j];
+          *reinterpret_cast<raw16_t*>(mine + TB + v_off<D>(r, ch)) = vw[j];
           if (kFp8 && ch == 0) { sc[r] = s0[j] * sl2e; sc[TK + r] = s1[j]; }
         }
       }
@@ -798,12 +765,6 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_partial_kernel(
   const TreeUnit u = tree_unit(th, tt.unit0, s, blockIdx.x);
   if (QGR == QGK || !u.ring) tree_body<KV, D, QGR>(c, th, tt, u, s, sl2e, parent, q, k_new, v_new, part, lds);
   else tree_body<KV, D, QGK>(c, th, tt, u, s, sl2e, parent, q, k_new, v_new, part, lds);
-}
-
-// 2^d for d <= 0, the whole part taken off first so that a difference of hundreds keeps its fraction
-__device__ __forceinline__ float tree_exp2(double d) {
-  const double whole = rint(d);
-  return ldexpf(__builtin_amdgcn_exp2f((float)(d - whole)), whole < -200.0 ? -200 : (int)whole);
 }
 
 // The same for fp32 rows, which come from memory to the operands: a wave has tiles of 16 keys and the workgroup 16 queries.  Logits
@@ -920,7 +881,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_partial_f32_kernel(
     const double ref = m == -INFINITY ? 0.0 : m;
     float p[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) p[r] = see[r] && xs[r] != -INFINITY ? tree_exp2(xs[r] - ref) : 0.f;
+    for (int r = 0; r < 4; ++r) p[r] = see[r] && xs[r] != -INFINITY ? exp2_diff(xs[r] - ref) : 0.f;
     l = fmaf(l, corr, (p[0] + p[1]) + (p[2] + p[3]));
     f32x4_t ot[SB];
 #pragma unroll
