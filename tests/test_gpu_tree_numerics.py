@@ -1,5 +1,5 @@
 """Drafted trees where the other tests' tolerances say little: logits of any size, weights in as many bits as a decode step holds them
-in."""
+in, every row of a unit counted once, and node rows of any alignment in an accepted path."""
 import numpy as np
 import pytest
 import torch
@@ -163,3 +163,96 @@ def test_a_tree_of_one_node_is_as_exact_as_a_decode_step(tb, bufs, rows, share):
         off = np.abs(x.double().cpu().numpy() - want[:, 0]) / tol[:, 0]
         print("%s: worst error over tolerance %.3f" % (name, off.max()), flush=True)
         assert off.max() <= 1.0
+
+
+# ------------------------------------------------------------------------------------------------ every row once --
+EVERY = [
+    # shape, lengths, nodes, rows kept: chunks of every length, windows and regions that end inside tiles and chunks
+    (shape(4, 2, 128, 16, 160, "bf16"), (5000, 1999, 161), 9, 0.5),
+    (shape(4, 1, 64, 16, 640, "bf16"), (640, 700, 1279, 639, 120, 2000), 40, 0.5),
+    (shape(8, 1, 128, 16, 384, "bf16", True), (2500, 385), 33, 0.6),
+    (shape(2, 1, 64, 16, 64, "bf16"), (21000,), 5, 0.6),
+    (shape(4, 2, 128, 16, 160, "fp8"), (5000, 1999, 161), 9, 0.5),
+    (shape(8, 1, 64, 16, 640, "fp8", True), (640, 1279, 639, 2000), 40, 0.5),
+    (shape(4, 2, 128, 16, 160, "f32"), (2600, 161), 9, 0.6),
+    (shape(4, 1, 64, 16, 640, "f32"), (640, 1279, 639, 2000), 24, 0.5),
+    (shape(2, 1, 64, 16, 64, "f32"), (13000,), 5, 0.6),
+]
+
+
+@pytest.mark.parametrize("i", range(len(EVERY)))
+def test_every_row_counts_once(tb, bufs, i):
+    """Nearly even weights, and V rows that are columns of a unit matrix (in long regions those next to a chunk's end, the others zero):
+    an element of the result is the sum of the weights of its column's rows, of which one too many or too few is more than the tolerance."""
+    case, lengths, n, fill = EVERY[i]
+    print("case", EVERY[i], flush=True)
+    d, w, fp8 = case["d"], case["w"], case["rows"] == "fp8"
+    prm, c = R.filled_cache(tb, bufs, case, lengths, 740 + i, room=37 * (i % 3), fill=fill)
+    if fp8:                                                              # K between 1/8 and 2, scales of 1
+        g = torch.Generator(device="cuda").manual_seed(i)
+        for t in (c.Kg, c.ringK):
+            t.copy_(torch.randint(0x20, 0x40, t.shape, device="cuda", generator=g))
+        for t in (c.Kg_scale, c.Vg_scale, c.ringK_scale, c.ringV_scale):
+            t.fill_(1.0)
+    q, k, v, parent = R.draft(case, len(lengths), n, 750 + i, [forked(n)] * len(lengths))
+    q = (q.float() / (32 * d ** 0.5)).to(q.dtype)
+    # a region's row r, counted from its head's first, and the ring's slot r in column r mod d; node r in column - r - 1
+    in_head = torch.cat([torch.arange(int(r), device="cuda") for r in np.diff(c.offs)])
+    far = (in_head + 24) % 4096 > 48 if max(lengths) > 10000 else torch.zeros_like(in_head, dtype=torch.bool)
+    for s, T in enumerate(lengths):
+        for h in range(c.n_rows.shape[1]):                               # the rows around the window's edge and the last ones
+            o, rows = int(c.offs[h]), int(c.n_rows[s, h])
+            edge = int((c.idx[s, o:o + rows] <= T - w).sum())
+            far[o + max(0, edge - 24):o + rows] = False
+    for t in (c.Vg, c.ringV):
+        at = in_head if t is c.Vg else torch.arange(w, device="cuda")
+        t.zero_()
+        t.scatter_(-1, (at % d).expand(t.shape[:-1])[..., None], 0x38 if fp8 else 1.0)              # (E4M3: 0x38 is 1)
+    c.Vg[:, :len(far)][:, far] = 0
+    v.zero_()
+    v.scatter_(-1, (d - 1 - torch.arange(n, device="cuda"))[None, :, None, None].expand(*v.shape[:3], 1), 1.0)
+    want, lightest = np.empty(q.shape), 1.0
+    for at, p, vals, _ in visible(case, c, q, k, v, parent):
+        want[at] = p @ vals
+        one = vals.any(1)
+        lightest = min(lightest, ((p * vals.max(1))[one] / want[at][vals.argmax(1)[one]]).min())
+    # A sum of weights, none negative: off by 2^-17 of itself for theirs, by their sums' roundings (numerator and denominator), by twice
+    # the logits' error (they are below 1/4, and so is the sum of their terms' magnitudes over 4: d 2^-24), and by the result's rounding.
+    most = int(c.n_rows.max()) + w + n
+    rel = (0.0 if case["rows"] == "f32" else 2.0 ** -8) + 2.0 ** -17 + 2 * d * 2.0 ** -24 + 2 * (most + 8) * 2.0 ** -24
+    print("lightest row %.4f of its column, tolerance %.4f" % (lightest, rel), flush=True)
+    assert lightest > 2 * rel
+    for size in (None, len(lengths) * n * case["hq"] * (2 + int(c.max_head_rows) // 4096) * (d + 4) * 4 + 256):
+        got = attend(tb, bufs, prm, c, q, k, v, parent, ws_bytes=size).double().cpu().numpy()
+        off = np.abs(got - want) - rel * want
+        print("worst %.3g" % off.max(), flush=True)
+        assert (off <= 0).all()
+
+
+# --------------------------------------------------------------------------------------- node rows of any alignment --
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,share", [("bf16", False), ("bf16", True), ("fp8", False), ("fp8", True), ("f32", False)])
+def test_accepted_rows_of_any_alignment(tb, bufs, rows, share, d):
+    """Acceptance takes q, k_new and v_new at any address of their type, one after the other and all at once, and leaves the same bytes."""
+    case = shape(4, 2, d, 8, 64, rows, share)
+    prm, c = R.filled_cache(tb, bufs, case, (200, 63, 5), 771)
+    n = 30
+    q, k, v, parent = R.draft(case, 3, n, 772, [list(range(-1, n - 1))] * 3)
+    last = torch.tensor([29, 12, 20], dtype=torch.int32, device="cuda")
+    P = np.stack([tb.tca_config_from_budget(8, 1.0, 0.4)] * tb.tca_selection_heads(prm))
+
+    def moved(x):
+        flat = torch.empty(x.numel() + 1, dtype=x.dtype, device="cuda")[1:]
+        y = flat.view(x.shape)
+        y.copy_(x)
+        assert y.data_ptr() % 16 == x.element_size()
+        return y
+
+    want = R.clone_cache(tb, bufs, prm, c)
+    tb.tca_tree_accept(prm, want.view, want.offs, n, parent, last, q, k, v, P)
+    for which in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 1)):
+        got = R.clone_cache(tb, bufs, prm, c)
+        rows_in = [moved(x) if m else x for x, m in zip((q, k, v), which)]
+        tb.tca_tree_accept(prm, got.view, got.offs, n, parent, last, *rows_in, P)
+        torch.cuda.synchronize()
+        assert not R.same_cache(got, want), which
