@@ -15,7 +15,7 @@
  *     ordinary CPU memory owned by the caller.  The library never allocates or
  *     frees device memory.  Scratch comes in through (ws, ws_bytes); query the
  *     size with the matching tca_*_workspace_bytes().  ws must be 256-byte aligned.
- *     tca_prefill and tca_decode also take less, down to a size that
+ *     tca_prefill, tca_decode and tca_decode_tree also take less, down to a size that
  *     tca_last_error() names after TCA_ERR_WORKSPACE: what they leave out is room to
  *     cut a call of few workgroups into more of them.  Such a call is slower, and as
  *     its sums are formed in another order its results may differ in the last bits.
@@ -195,7 +195,9 @@ int tca_select(const tca_params* prm, const void* q_last, const void* K, const v
  *   lse    : device float [Hq, n_queries] or NULL: natural-log sum of exp of the scaled logits
  * Kg and Vg may both be NULL (gather-free call): the global rows are read from K and V through
  * idx, for a prefill whose kept rows are not needed afterwards as a compacted cache.
- * TCA_BF16: bf16 MFMA products, fp32 softmax and accumulation.  TCA_F32: fp64 logits, fp32
+ * TCA_BF16: bf16 MFMA products, fp32 softmax and accumulation, the softmax weights rounded to bf16 for the
+ * product with V; logits up to about 1e6 (an exponent is the difference of two fp32 products, which beyond that
+ * no longer holds to a fraction of one: far beyond it rows come out as zero or NaN).  TCA_F32: fp64 logits, fp32
  * exponentials and accumulation.
  * TCA_BF16 limit: (q_pos0 + n_queries + w + 128) * d * 2 bytes and every head's region must stay
  * below 2 GiB (8M positions at d = 128); beyond that the call returns TCA_ERR_UNSUPPORTED.
@@ -253,8 +255,10 @@ int tca_select_prefill_overlapped(const tca_params* prm, const void* q_last, con
  * Row i of a prompt attends to rows 0 .. i of that prompt.  Rows of O and lse outside the prompts are
  * left as they are.  Of prm only the head counts, head_dim, dtype and scale have a part in it.
  * Q, K, V, O must be 16-byte aligned.  TCA_BF16: a prompt has at most 2^31 / (2 d) - 256 rows.
- * Arithmetic as for tca_prefill.  A row of V that is not finite reaches the queries that see it and
- * no others.  Takes no workspace; does not synchronise; one launch for up to 96 prompts. */
+ * Arithmetic and bounds of the logits as for tca_prefill.  A row of V that is not finite reaches the queries
+ * that see it and no others; for that (TCA_BF16) all of a prompt from the 32 rows around it on is formed again
+ * key by key, which takes some thirty times as long.  A prompt's keys are not split: a call of few heads and
+ * one prompt of thousands of rows takes up to a fifth longer than tca_prefill.  Takes no workspace; does not synchronise; one launch for up to 96 prompts. */
 int tca_prefill_packed(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t stride,
                        int n_seqs, const int64_t* seq_offs, void* O, float* lse, void* stream);
 
@@ -373,7 +377,8 @@ int tca_decode_static(const tca_params* prm, const tca_cache* cache, const int64
  * that is none: nothing is).  The nodes of the path enter the cache in order, as tca_decode enters its
  * rows: ring slots, lengths, and for every block that is complete with one of them the selection
  * with that node's queries (q, k_new, v_new, p as above and for tca_decode).  The cache is then, bit
- * for bit, as the same steps of tca_decode leave it.  The lengths must be below 2^48.
+ * for bit, as the same steps of tca_decode leave it.  The lengths must be below 2^48.  While the call runs, a
+ * length's word may hold neither the old nor the new number (its high bits count): what reads it waits for the call.
  *
  * Neither call synchronises, allocates or sets memory; both may be captured into a HIP graph. */
 size_t tca_decode_tree_workspace_bytes(const tca_params* prm, int batch, int n_nodes, int64_t max_head_rows);
