@@ -1,8 +1,8 @@
 // Copies of whole sequences inside a decode cache or from one cache to another: forks, compaction of a batch, a move to a
 // cache with other capacities, and slots made empty.
 //
-// HBM-bound: 5.5 TB/s, read and written together.  A region's or ring's rows lie one behind the other, so a unit of work (kUnitBytes of one head's K rows and of its
-// V rows) is a piece of memory.  It is requested whole into registers and stored to every copy that the launch makes of
+// HBM-bound: 5.1 to 5.8 TB/s, read and written together.  A region's or ring's rows lie one behind the other, so a unit of work (kUnitBytes of
+// one head's K rows and of its V rows) is a piece of memory.  It is requested whole into registers and stored to every copy that the launch makes of
 // its sequence, so that a fork reads its source once.  The host does not know how full a region is: there is a unit for every
 // kUnitBytes of the smaller capacity, and those behind the last row return at once.
 #include <hip/hip_runtime.h>

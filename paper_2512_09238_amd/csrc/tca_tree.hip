@@ -12,9 +12,9 @@
 // Up to 64 queries a row the memory is the bound: a row of K and V (512 bytes at d = 128, bf16) takes 64 x 768 flops, a fifth of
 // what the matrix cores do in the time that its bytes take.  So the shape follows the loads: tiles are copied straight into LDS ahead
 // of their use, a wave with a tile of its own needs no barrier, and two workgroups a CU cover each other's start and end.  32 heads,
-// d = 128, budgets of 27 % on average: 64 nodes over 16 x 100000 tokens 1.01 to 1.02 ms, 4.9 TB/s; 8 over 16 x
-// 60000 514 us, 5.8 TB/s; 32 over 8 x 30000 173 us, 4.4 TB/s (a tenth of it in the rings, whose rows meet 128 queries); 5 over
-// 1 x 2000 15 us, of which the two launches, each a chain of waits, are all.  (A first shape, a wave with up to 64 queries and masks in
+// d = 128, budgets of 27 % on average: 64 nodes over 16 x 100000 tokens 1.01 to 1.02 ms, 4.8 to 4.9 TB/s; 8 over 16 x
+// 60000 514 us, 5.8 TB/s; 32 over 8 x 30000 173 to 174 us, 4.4 TB/s (a tenth of it in the rings, whose rows meet 128 queries); 5 over
+// 1 x 2000 15 to 17 us, of which the two launches, each a chain of waits, are all.  (A first shape, a wave with up to 64 queries and masks in
 // every tile: 1730 us, 283 us and 21 us for the first, third and last.)
 // With 128 queries a row, on the FP8 cache (half the bytes), the products and weights are the bound: 16 nodes of 8 heads over 12 x
 // 60000 tokens 222 to 235 us, where their bytes take 85 and their products 95.  A round of 128 queries and 64 keys takes two
